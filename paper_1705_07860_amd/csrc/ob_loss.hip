@@ -163,7 +163,8 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS) k_
     }
     if (own == low) s = s == s ? 0.0f : s, w = 0.0f;       // nothing seen, or only NaN
     else {
-        const float by = __expf(own - m), d = own - m;
+        // bounded as above: with all of a thread's scores at the type's lowest value d * s passes fp32's range where by is 0
+        const float by = __expf(own - m), d = fmaxf(own - m, -1e30f);
         w = by * (w + d * s);
         s *= by;
     }
@@ -329,7 +330,8 @@ template <typename T> __global__ void __launch_bounds__(256) k_logprobs_grad(con
     const float b = A.dentropy ? A.dentropy[row] : 0.0f;
     if (label >= A.classes) a = __builtin_nanf("");
     const bool empty = sum == 0.0f;
-    const float inv = 1.0f / sum, log_sum = logf(sum), ab = a + b * (h - log_sum);
+    // without a gradient of the entropy, the entropy has no part (a row that is not finite has a sum of NaN)
+    const float inv = 1.0f / sum, log_sum = logf(sum), ab = b == 0.0f ? a : a + b * (h - log_sum);
     const int full = A.classes / VEC, vecs = (A.classes + VEC - 1) / VEC;
     const int v0 = (int)blockIdx.y * A.piece, v1 = min(vecs, v0 + A.piece);
     auto grad = [&](float v, int c) {
