@@ -136,8 +136,10 @@ __global__ void __launch_bounds__(256) k_update(const UpdateArgs A)
     for (int i = (int)threadIdx.x; i < A.part_count; i += 256) sum += A.part[i];
     const double norm = sqrt(block_sum(sum, s_part));
     if (A.norm && blockIdx.x == 0 && threadIdx.x == 0) *A.norm = (float)norm;
+    // no limit and an infinite norm clip nothing, nor do zeros; a norm of NaN makes NaN of everything, whatever the limit is
     double by = A.max_norm / norm;
-    if (by > 1.0 || A.max_norm == __builtin_inf() || norm == 0.0) by = 1.0;        // a NaN stays one
+    if (norm != norm) by = norm;
+    else if (by > 1.0 || A.max_norm == __builtin_inf() || norm == 0.0) by = 1.0;
     const float rate = (float)(by * A.lr);
     const u32 chunks = A.cum[A.n];
     if (A.clip_grads && rate == 1.0f) return;
