@@ -631,16 +631,21 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
 #pragma unroll
                 for (int ct = 0; ct < NC; ++ct) x0[ct] *= held, x1[ct] *= held;
             }
-            if constexpr (STATE_ONLY) {             // the rows behind the chunk
-                const float behind = decay_power(decay, at);
+            // The rows behind the chunk.  A type of fp32's range takes their decay before it is split into terms; fp16 would lose what has decayed
+            // below its own range, so its products are made of rows as they are and decayed as they are added, in fp32.
+            float behind = 1.0f;
+            if constexpr (STATE_ONLY) {
+                behind = decay_power(decay, at);
+                if constexpr (Q::SCALED) behind *= two_to(-s_scale);
+                else
 #pragma unroll
-                for (int ct = 0; ct < NC; ++ct) x0[ct] *= behind, x1[ct] *= behind;
+                    for (int ct = 0; ct < NC; ++ct) x0[ct] *= behind, x1[ct] *= behind;
             }
+            if constexpr (!STATE_ONLY)
 #pragma unroll
-            for (int ct = 0; ct < NC; ++ct)
+                for (int ct = 0; ct < NC; ++ct)
 #pragma unroll
-                for (int dt = 0; dt < ND; ++dt)
-                    if (!STATE_ONLY || Q::SCALED) S[ct][dt] *= keep;
+                    for (int dt = 0; dt < ND; ++dt) S[ct][dt] *= keep;
             constexpr int M = Q::SPLIT < 2 ? 1 : 2;
             Frag t0[NC][M], t1[NC][M];
 #pragma unroll
@@ -655,13 +660,25 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
             for (int dt = 0; dt < ND; dt += 2) {
                 const Frag u0 = b_cols(0, dt * 16), u1 = b_cols(16, dt * 16);
                 const Frag z0 = b_cols(0, dt * 16 + 16), z1 = b_cols(16, dt * 16 + 16);
+                if constexpr (STATE_ONLY && Q::SCALED) {
+                    f4 y[NC][2] = {};
 #pragma unroll
-                for (int m = 0; m < M; ++m)
+                    for (int m = 0; m < M; ++m)
 #pragma unroll
-                    for (int ct = 0; ct < NC; ++ct) {
-                        S[ct][dt] = Q::mma(u0, u1, t0[ct][m], t1[ct][m], S[ct][dt]);
-                        S[ct][dt + 1] = Q::mma(z0, z1, t0[ct][m], t1[ct][m], S[ct][dt + 1]);
-                    }
+                        for (int ct = 0; ct < NC; ++ct) {
+                            y[ct][0] = Q::mma(u0, u1, t0[ct][m], t1[ct][m], y[ct][0]);
+                            y[ct][1] = Q::mma(z0, z1, t0[ct][m], t1[ct][m], y[ct][1]);
+                        }
+#pragma unroll
+                    for (int ct = 0; ct < NC; ++ct) S[ct][dt] += y[ct][0] * behind, S[ct][dt + 1] += y[ct][1] * behind;
+                } else
+#pragma unroll
+                    for (int m = 0; m < M; ++m)
+#pragma unroll
+                        for (int ct = 0; ct < NC; ++ct) {
+                            S[ct][dt] = Q::mma(u0, u1, t0[ct][m], t1[ct][m], S[ct][dt]);
+                            S[ct][dt + 1] = Q::mma(z0, z1, t0[ct][m], t1[ct][m], S[ct][dt + 1]);
+                        }
             }
             if constexpr (Q::SPLIT > 2) {
                 if (exact) {
@@ -731,7 +748,7 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
         if constexpr (BUF == 1) __syncthreads();
     }
     if (STATE_ONLY || give) {
-        const float by = Q::SCALED ? two_to(-s_scale) : 1.0f;
+        const float by = !STATE_ONLY && Q::SCALED ? two_to(-s_scale) : 1.0f;
 #pragma unroll
         for (int ct = 0; ct < NC; ++ct)
 #pragma unroll
