@@ -160,6 +160,13 @@ __device__ __forceinline__ int wave_max(int x)
     return max(a, b);
 }
 __device__ __forceinline__ int bits_of(float x) { return __builtin_bit_cast(int, __builtin_fabsf(x)); }
+constexpr int BITS_INF = 0x7f800000;
+// the same, 0 of what is no finite number: a range is that of the finite ones, which an infinity beside them may not push out of fp16
+__device__ __forceinline__ int finite_bits(float x)
+{
+    const int b = bits_of(x);
+    return b < BITS_INF ? b : 0;
+}
 // the power of two that brings a magnitude (its bits) to 2^11 .. 2^12, as an exponent: products keep 26 binary places below the largest
 __device__ __forceinline__ int fit_exponent(int bits)
 {
@@ -558,7 +565,7 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
                     const float most = fmaxf(fmaxf(fabsf(x[0]), fabsf(x[1])), fmaxf(fabsf(x[2]), fabsf(x[3])));
                     int e = 0;
                     if (__builtin_amdgcn_ballot_w64(most > 32768.0f) || !__builtin_amdgcn_ballot_w64(most >= 0.125f)) {
-                        e = fit_exponent(wave_max(bits_of(most)));
+                        e = fit_exponent(wave_max(max(max(finite_bits(x[0]), finite_bits(x[1])), max(finite_bits(x[2]), finite_bits(x[3])))));
                         x *= two_to(e);
                     }
                     if (lane == 0) s_exp[half][t] = e;
@@ -593,7 +600,18 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
 #pragma unroll
                             for (int r = 0; r < 4; r += 2) most = fmaxf(most, fabsf(S[ct][dt][r]) + fabsf(S[ct][dt][r + 1]));
                     if (__builtin_amdgcn_ballot_w64(most > 32768.0f) || !__builtin_amdgcn_ballot_w64(most >= 1.0f)) {
-                        const int e = fit_exponent(wave_max(bits_of(most)));
+                        int bits = wave_max(bits_of(most));
+                        if (bits >= BITS_INF) {
+                            bits = 0;
+#pragma unroll
+                            for (int ct = 0; ct < NC; ++ct)
+#pragma unroll
+                                for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                                    for (int r = 0; r < 4; ++r) bits = max(bits, finite_bits(S[ct][dt][r]));
+                            bits = wave_max(bits);
+                        }
+                        const int e = fit_exponent(bits);
                         by_state = two_to(-e - s_scale);
                         from_state(std::true_type(), two_to(e));
                     } else
@@ -622,7 +640,15 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
                 // held times 2^s_scale, the largest between 2^11 and 2^14: the second term has its bits then down to 2^-24 of the largest
                 most_x *= held;
                 if (__builtin_amdgcn_ballot_w64(most_x > 16384.0f) || !__builtin_amdgcn_ballot_w64(most_x >= 2048.0f)) {
-                    const int bits = wave_max(bits_of(most_x));
+                    int bits = wave_max(bits_of(most_x));
+                    if (bits >= BITS_INF) {
+                        bits = 0;
+#pragma unroll
+                        for (int ct = 0; ct < NC; ++ct)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) bits = max(bits, max(finite_bits(x0[ct][r] * held), finite_bits(x1[ct][r] * held)));
+                        bits = wave_max(bits);
+                    }
                     if (bits) {
                         const int e = min(max(fit_exponent(bits), -100 - s_scale), 100 - s_scale);
                         keep *= two_to(e), held *= two_to(e), s_scale += e;
