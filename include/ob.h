@@ -113,7 +113,8 @@ int ob_ctx_set_launch(ob_ctx *ctx, int launch);
  * dependency path then share the launches next to their consumers).  Other values: OB_E_ARG. */
 int ob_ctx_set_fusion(ob_ctx *ctx, int on);
 /* Library-owned message for the last failing call on this context (valid until the next
- * call); ctx may be NULL for errors of ob_ctx_create. */
+ * call); ctx may be NULL for errors of ob_ctx_create and of the calls without a context: each host
+ * thread has its own message of these. */
 const char *ob_last_error(ob_ctx *ctx);
 
 /* ---- parameters (persist across graphs) ------------------------------------------------- */

@@ -14,7 +14,8 @@
 #include <new>
 #include <thread>
 
-static std::string g_create_error;
+// the message of the last failed call without a context, each host thread its own
+static thread_local char g_error[512];
 
 // Three helper threads for the bulk hand-over of large graphs, started on first use and kept for
 // the life of the process (starting threads per call costs more than the work they take over).
@@ -78,7 +79,7 @@ int ctx_fail(ob_ctx *ctx, int code, const char *fmt, ...)
     va_start(ap, fmt);
     vsnprintf(buf, sizeof buf, fmt, ap);
     va_end(ap);
-    if (ctx) ctx->err = buf; else g_create_error = buf;
+    if (ctx) ctx->err = buf; else snprintf(g_error, sizeof g_error, "%s", buf);
     return code;
 }
 
@@ -97,7 +98,7 @@ void *arena_alloc(ob_ctx *ctx, size_t bytes)
 
 extern "C" {
 
-const char *ob_last_error(ob_ctx *ctx) { return ctx ? ctx->err.c_str() : g_create_error.c_str(); }
+const char *ob_last_error(ob_ctx *ctx) { return ctx ? ctx->err.c_str() : g_error; }
 
 int ob_ctx_create(void *arena_dev, size_t arena_bytes, void *hip_stream, ob_ctx **out)
 {
