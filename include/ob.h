@@ -322,7 +322,8 @@ int ob_test_gemm(ob_ctx *ctx, int M, int N, int K, const float *A, const float *
 #define OB_TYPE_FP16 2
 
 /* rows of heads: element e of head h of token t is data[t * token_stride + h * head_stride + e]; strides in
- * elements, not negative, less than 2^24 from token to token; any alignment of the element */
+ * elements, not negative; less than 2^24 from token to token where the rows of several tokens are walked (not in
+ * ob_decay_attention_step); any alignment of the element */
 typedef struct ob_rows {
     void *data;
     int64_t token_stride, head_stride;

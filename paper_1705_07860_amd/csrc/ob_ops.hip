@@ -147,8 +147,10 @@ static int check_decay(const ob_decay *p, const char *who, bool packed)
     if (p->n_seqs < 0 || p->tokens < 0 || p->tokens > 0x7fffffff) return ops_fail(OB_E_RANGE, "%s: %d sequences, %lld tokens", who, p->n_seqs, (long long)p->tokens);
     if (p->n_seqs && !p->log_decay) return ops_fail(OB_E_ARG, "%s: no decay", who);
     if (p->tokens && (!p->q.data || !p->k.data || !p->v.data || !p->o.data)) return ops_fail(OB_E_ARG, "%s: null array", who);
+    // a scan's places in a chunk are 32-bit offsets; single tokens' are 64 bits, and of one row the stride is not looked at
+    const bool walked = packed && p->tokens > 1;
     for (const ob_rows *r : {&p->q, &p->k, &p->v, &p->o, &p->dq, &p->dk_rows, &p->dv_rows})
-        if (r->token_stride < 0 || r->token_stride >= 1 << 24 || r->head_stride < 0)
+        if (r->token_stride < 0 || (walked && r->token_stride >= 1 << 24) || r->head_stride < 0)
             return ops_fail(OB_E_RANGE, "%s: strides of %lld and %lld elements", who, (long long)r->token_stride, (long long)r->head_stride);
     if (!packed) {
         if (p->tokens != p->n_seqs) return ops_fail(OB_E_DIM, "%s: %lld tokens of %d sequences", who, (long long)p->tokens, p->n_seqs);
@@ -249,6 +251,8 @@ static size_t part_bytes(const ob_decay *p)
 static int grad_scans(const ob_decay *p) { return pad_width(p->dk) == pad_width(p->dv) ? 3 : 2; }
 
 static Rows rows_of(const ob_rows &r, int div) { return Rows{r.data, r.token_stride, r.head_stride, div, 0}; }
+static i64 token_step(const ob_decay *p, const ob_rows &r) { return p->tokens > 1 ? r.token_stride : 0; }
+static Rows scan_rows(const ob_decay *p, const ob_rows &r, int div) { return Rows{r.data, token_step(p, r), r.head_stride, div, 0}; }
 
 static int scan_all(hipStream_t s, ScanArgs &A, const ob_decay *p, int segment)
 {
@@ -301,8 +305,8 @@ int ob_decay_attention(void *hip_stream, const ob_decay *p)
     ScanArgs A;
     A.n_scans = 1, A.heads = p->heads, A.log_decay = p->log_decay, A.slots = (float *)p->workspace;
     Scan &x = A.scan[0];
-    x.a = rows_of(p->q, 1), x.b = rows_of(p->k, group), x.c = rows_of(p->v, group);
-    x.y = p->o.data, x.y_token = p->o.token_stride, x.y_head = p->o.head_stride;
+    x.a = scan_rows(p, p->q, 1), x.b = scan_rows(p, p->k, group), x.c = scan_rows(p, p->v, group);
+    x.y = p->o.data, x.y_token = token_step(p, p->o), x.y_head = p->o.head_stride;
     x.s_in = p->state_in, x.s_out = p->state_out;
     x.sp = x.sy = (float)p->scale, x.ss = 1.0f;
     x.da = p->dk, x.dc = p->dv, x.s_row = p->dv, x.s_col = 1;
@@ -325,8 +329,8 @@ int ob_decay_attention_grad(void *hip_stream, const ob_decay *p)
     A.n_scans = scans, A.heads = p->heads, A.log_decay = p->log_decay, A.slots = (float *)p->workspace;
     // dq: the scan of do against v and k, on the transposed state
     Scan &q = A.scan[0], &k = A.scan[1];
-    q.a = rows_of(p->o, 1), q.b = rows_of(p->v, group), q.c = rows_of(p->k, group);
-    q.y = p->dq.data, q.y_token = p->dq.token_stride, q.y_head = p->dq.head_stride;
+    q.a = scan_rows(p, p->o, 1), q.b = scan_rows(p, p->v, group), q.c = scan_rows(p, p->k, group);
+    q.y = p->dq.data, q.y_token = token_step(p, p->dq), q.y_head = p->dq.head_stride;
     q.s_in = p->state_in, q.s_out = nullptr;
     q.sp = q.sy = (float)p->scale, q.ss = 1.0f;
     q.da = p->dv, q.dc = p->dk, q.s_row = 1, q.s_col = p->dv;
@@ -337,11 +341,11 @@ int ob_decay_attention_grad(void *hip_stream, const ob_decay *p)
     k.sp = k.ss = (float)p->scale, k.sy = 1.0f;
     k.s_in = p->dstate_out;
     Scan v = k;
-    k.a = rows_of(p->v, group), k.b = rows_of(p->o, 1), k.c = rows_of(p->q, 1);
-    k.y = p->dk_rows.data, k.y_token = p->dk_rows.token_stride, k.y_head = p->dk_rows.head_stride;
+    k.a = scan_rows(p, p->v, group), k.b = scan_rows(p, p->o, 1), k.c = scan_rows(p, p->q, 1);
+    k.y = p->dk_rows.data, k.y_token = token_step(p, p->dk_rows), k.y_head = p->dk_rows.head_stride;
     if (group > 1) k.y = part_k, k.y_token = (i64)p->heads * p->dk, k.y_head = p->dk;
-    v.a = rows_of(p->k, group), v.b = rows_of(p->q, 1), v.c = rows_of(p->o, 1);
-    v.y = p->dv_rows.data, v.y_token = p->dv_rows.token_stride, v.y_head = p->dv_rows.head_stride;
+    v.a = scan_rows(p, p->k, group), v.b = scan_rows(p, p->q, 1), v.c = scan_rows(p, p->o, 1);
+    v.y = p->dv_rows.data, v.y_token = token_step(p, p->dv_rows), v.y_head = p->dv_rows.head_stride;
     if (group > 1) v.y = part_v, v.y_token = (i64)p->heads * p->dv, v.y_head = p->dv;
     v.da = p->dk, v.dc = p->dv, v.s_row = p->dv, v.s_col = 1;
     v.s_out = p->dstate_in, v.exact_state = p->dstate_in != nullptr;
