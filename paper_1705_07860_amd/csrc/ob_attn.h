@@ -828,7 +828,9 @@ int scan_f16(hipStream_t, const ScanArgs &, int group);
 template <typename T, int DA, int DC, bool FULL> static int scan_launch(hipStream_t s, const ScanArgs &A, int group)
 {
     const int each = A.n_scans * (A.heads / group);
-    const dim3 grid((unsigned)((A.n_units * each + 7) / 8 * 8 * group)), block(64 * scan_waves<DC>());
+    const i64 blocks = ((i64)A.n_units * each + 7) / 8 * 8 * group;
+    if (!launch_fits(blocks, 64 * scan_waves<DC>())) return ops_fail(OB_E_RANGE, "decay attention: %d units of %d heads in one launch", A.n_units, A.heads);
+    const dim3 grid((unsigned)blocks), block(64 * scan_waves<DC>());
     if (A.n_split) {
         const int cut = A.n_cut * each;                                 // the units of cut sequences come first
         k_scan<T, DA, DC, true, FULL><<<dim3((unsigned)((cut + 7) / 8 * 8 * group)), block, 0, s>>>(A, group);

@@ -38,3 +38,5 @@ static inline int ops_launched(const char *what)
     const hipError_t e = hipGetLastError();
     return e == hipSuccess ? OB_OK : ops_fail(OB_E_HIP, "%s: %s", what, hipGetErrorString(e));
 }
+// threads of a launch along one axis are counted in 32 bits
+static inline bool launch_fits(i64 blocks, int threads) { return blocks <= 0xffffffffll / threads; }

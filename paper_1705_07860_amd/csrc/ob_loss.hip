@@ -9,7 +9,7 @@ struct ScoreArgs {
     i64 x_row;                      // elements between rows
     const void *labels;
     int labels_wide;                // 64 bits
-    int rows, classes, top;
+    int first, rows, classes, top;  // rows of one launch, from `first` on
     float *logprob, *entropy, *row_max, *row_sum, *top_logprob;
     int *top_id;
 };
@@ -57,7 +57,7 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS) k_
     typedef u32 Raw __attribute__((ext_vector_type(4)));
     struct __attribute__((packed, aligned(sizeof(T)))) RawAt { Raw v; };
     __shared__ float s_red[3][WAVES];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = A.first + (int)blockIdx.x;
     const T *first = (const T *)A.x + row * A.x_row;
     // vectors from the first place of 16 bytes on (rows of 50 257 bf16: 82 us for 93); what lies before it goes one by one
     const int head = min((int)(-(uintptr_t)first & 15) / (int)sizeof(T), A.classes), classes = A.classes - head;
@@ -290,17 +290,22 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS) k_
     }
 }
 
-template <typename T> int logprobs_launch(hipStream_t s, const ScoreArgs &A)
+constexpr int ROWS = 1 << 21;        // of one launch: 1024 threads each stay below 2^32
+
+template <typename T> int logprobs_launch(hipStream_t s, ScoreArgs &A, int rows)
 {
     constexpr int VEC = 16 / (int)sizeof(T);
     const int vecs = (A.classes + VEC - 1) / VEC;
     // eight vectors a thread; where there are fewer rows than compute units a row's latency is all that counts: two
-    const dim3 grid((unsigned)A.rows);
-    const int want = A.rows <= 256 ? vecs / 2 : vecs / 8;
-    if (want <= 64) k_logprobs<T, 64><<<grid, 64, 0, s>>>(A);
-    else if (want <= 256) k_logprobs<T, 256><<<grid, 256, 0, s>>>(A);
-    else if (want <= 512) k_logprobs<T, 512><<<grid, 512, 0, s>>>(A);
-    else k_logprobs<T, 1024><<<grid, 1024, 0, s>>>(A);
+    const int want = rows <= 256 ? vecs / 2 : vecs / 8;
+    for (A.first = 0; A.first < rows; A.first += A.rows) {
+        A.rows = rows - A.first < ROWS ? rows - A.first : ROWS;
+        const dim3 grid((unsigned)A.rows);
+        if (want <= 64) k_logprobs<T, 64><<<grid, 64, 0, s>>>(A);
+        else if (want <= 256) k_logprobs<T, 256><<<grid, 256, 0, s>>>(A);
+        else if (want <= 512) k_logprobs<T, 512><<<grid, 512, 0, s>>>(A);
+        else k_logprobs<T, 1024><<<grid, 1024, 0, s>>>(A);
+    }
     return ops_launched("ob_token_logprobs");
 }
 
@@ -308,7 +313,7 @@ struct ScoreGradArgs {
     const void *x;
     i64 x_row;
     const void *labels;
-    int labels_wide, rows, classes, piece;      // piece: vectors of a row for one workgroup
+    int labels_wide, first, rows, classes, piece;      // rows of one launch, from `first` on; piece: vectors of a row for one workgroup
     const float *row_max, *row_sum, *entropy, *dlogprob, *dentropy;
     void *dx;
     i64 dx_row;
@@ -320,7 +325,7 @@ template <typename T> __global__ void __launch_bounds__(256) k_logprobs_grad(con
 {
     constexpr int VEC = 16 / (int)sizeof(T), U = 4;
     typedef typename Pack<T, VEC>::V V;
-    const int row = A.rows - 1 - (int)blockIdx.x;
+    const int row = A.first + A.rows - 1 - (int)blockIdx.x;
     const T *x = (const T *)A.x + row * A.x_row;
     T *dx = (T *)A.dx + row * A.dx_row;
     const i64 label = label_of(A.labels, A.labels_wide, row);
@@ -361,15 +366,18 @@ template <typename T> __global__ void __launch_bounds__(256) k_logprobs_grad(con
     }
 }
 
-template <typename T> int grad_launch(hipStream_t s, ScoreGradArgs &A)
+template <typename T> int grad_launch(hipStream_t s, ScoreGradArgs &A, int rows)
 {
     constexpr int VEC = 16 / (int)sizeof(T);
     const int vecs = (A.classes + VEC - 1) / VEC;
     // a workgroup has a whole row where there are rows enough for the chip, else a piece of one
     int pieces = 1;
-    while (pieces < 64 && (i64)A.rows * pieces < 1024 && vecs > 256 * pieces) pieces *= 2;
+    while (pieces < 64 && (i64)rows * pieces < 1024 && vecs > 256 * pieces) pieces *= 2;
     A.piece = (vecs + pieces - 1) / pieces;
-    k_logprobs_grad<T><<<dim3((unsigned)A.rows, (unsigned)pieces), 256, 0, s>>>(A);
+    for (int end = rows; end; end = A.first) {                  // the last rows first, here too
+        A.first = end > ROWS ? end - ROWS : 0, A.rows = end - A.first;
+        k_logprobs_grad<T><<<dim3((unsigned)A.rows, (unsigned)pieces), 256, 0, s>>>(A);
+    }
     return ops_launched("ob_token_logprobs_grad");
 }
 
@@ -394,11 +402,11 @@ int ob_token_logprobs(void *hip_stream, const ob_logprobs *p)
     if (!p->rows) return OB_OK;
     ScoreArgs A;
     A.x = p->scores, A.x_row = p->score_stride, A.labels = p->labels, A.labels_wide = p->labels_wide;
-    A.rows = p->rows, A.classes = p->classes, A.top = p->top;
+    A.first = 0, A.rows = 0, A.classes = p->classes, A.top = p->top;
     A.logprob = p->logprob, A.entropy = p->entropy, A.row_max = p->row_max, A.row_sum = p->row_sum;
     A.top_logprob = p->top_logprobs, A.top_id = p->top_ids;
     hipStream_t s = (hipStream_t)hip_stream;
-    return p->type == OB_TYPE_FP32 ? logprobs_launch<float>(s, A) : p->type == OB_TYPE_BF16 ? logprobs_launch<bf16>(s, A) : logprobs_launch<f16>(s, A);
+    return p->type == OB_TYPE_FP32 ? logprobs_launch<float>(s, A, p->rows) : p->type == OB_TYPE_BF16 ? logprobs_launch<bf16>(s, A, p->rows) : logprobs_launch<f16>(s, A, p->rows);
 }
 
 int ob_token_logprobs_grad(void *hip_stream, const ob_logprobs *p)
@@ -408,11 +416,11 @@ int ob_token_logprobs_grad(void *hip_stream, const ob_logprobs *p)
     if (!p->rows) return OB_OK;
     ScoreGradArgs A;
     A.x = p->scores, A.x_row = p->score_stride, A.labels = p->labels, A.labels_wide = p->labels_wide;
-    A.rows = p->rows, A.classes = p->classes, A.piece = 0;
+    A.first = 0, A.rows = 0, A.classes = p->classes, A.piece = 0;
     A.row_max = p->row_max, A.row_sum = p->row_sum, A.entropy = p->entropy, A.dlogprob = p->dlogprob, A.dentropy = p->dentropy;
     A.dx = p->dscores, A.dx_row = p->dscore_stride;
     hipStream_t s = (hipStream_t)hip_stream;
-    return p->type == OB_TYPE_FP32 ? grad_launch<float>(s, A) : p->type == OB_TYPE_BF16 ? grad_launch<bf16>(s, A) : grad_launch<f16>(s, A);
+    return p->type == OB_TYPE_FP32 ? grad_launch<float>(s, A, p->rows) : p->type == OB_TYPE_BF16 ? grad_launch<bf16>(s, A, p->rows) : grad_launch<f16>(s, A, p->rows);
 }
 
 }  // extern "C"

@@ -95,6 +95,7 @@ template <typename T> static int step_launch(hipStream_t s, const StepArgs &A, i
     const int tx = A.dv <= 32 ? 8 : A.dv <= 64 ? 16 : 32;
     int threads = 64;
     while (threads < 256 && (threads < 4 * tx || 8 * (threads / tx) < A.dk)) threads *= 2;
+    if (!launch_fits((i64)n * A.heads, threads)) return ops_fail(OB_E_RANGE, "ob_decay_attention_step: %d sequences of %d heads", n, A.heads);
     const dim3 grid((unsigned)n * (unsigned)A.heads);
     if (tx == 8) k_step<T, 8><<<grid, threads, 0, s>>>(A);
     else if (tx == 16) k_step<T, 16><<<grid, threads, 0, s>>>(A);
@@ -274,7 +275,7 @@ static int sum_heads(hipStream_t s, const ob_decay *p, const float *dk, const fl
     if (!A.rows) return OB_OK;
     const int per = 256 / ((std::max(p->dk, p->dv) + 3) / 4);       // rows of a workgroup, at least
     const i64 blocks = (A.rows + per - 1) / per;
-    if (blocks > 0x7fffffff) return ops_fail(OB_E_RANGE, "ob_decay_attention_grad: %lld rows", (long long)A.rows);
+    if (!launch_fits(blocks, 256)) return ops_fail(OB_E_RANGE, "ob_decay_attention_grad: %lld rows", (long long)A.rows);
     const dim3 grid((unsigned)blocks, 2);
     if (p->type == OB_TYPE_FP32) k_sum_heads<float><<<grid, 256, 0, s>>>(A);
     else if (p->type == OB_TYPE_BF16) k_sum_heads<bf16><<<grid, 256, 0, s>>>(A);
@@ -363,7 +364,6 @@ int ob_decay_attention_step(void *hip_stream, const ob_decay *p)
     if (int rc = check_decay(p, "ob_decay_attention_step", false)) return rc;
     if (!p->n_seqs) return OB_OK;
     if (!p->state_out) return ops_fail(OB_E_ARG, "ob_decay_attention_step: no state");
-    if ((i64)p->n_seqs * p->heads > 0x7fffffff) return ops_fail(OB_E_RANGE, "ob_decay_attention_step: %d sequences of %d heads", p->n_seqs, p->heads);
     const int group = p->heads / p->kv_heads;
     StepArgs A;
     A.q = rows_of(p->q, 1), A.k = rows_of(p->k, group), A.v = rows_of(p->v, group);
