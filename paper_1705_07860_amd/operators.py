@@ -38,6 +38,13 @@ def _call(name, rc):
         raise ObError(rc, (lib().ob_last_error(None) or b"").decode() or name)
 
 
+def _packed(record, *args):
+    try:
+        return record.pack(*args)
+    except struct.error as e:
+        raise ObError(OB_E_RANGE, f"an argument does not fit: {e}")
+
+
 # torch.cuda.current_stream() builds an object (2.7 us); the address alone takes 0.1, against some 3 us of a launch
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
@@ -85,6 +92,8 @@ def _widths(q, k, v):
     kv_heads, dv = v.shape[1:]
     if heads < 1 or kv_heads < 1 or heads % kv_heads:
         raise ObError(OB_E_DIM, f"{heads} heads over {kv_heads} of keys and values")
+    if dk < 1 or dv < 1:
+        raise ObError(OB_E_DIM, f"widths {dk} and {dv}")
     return tokens, heads, kv_heads, dk, dv
 
 
@@ -135,10 +144,10 @@ def decay_attention(q, k, v, log_decay, offsets, scale: Optional[float] = None, 
             *_rows("q", q, (tokens, heads, dk), q.dtype), *_rows("k", k, (tokens, kv_heads, dk), q.dtype),
             *_rows("v", v, (tokens, kv_heads, dv), q.dtype), o.data_ptr(), heads * dv, dv, *_NO_ROWS, *_NO_ROWS, *_NO_ROWS,
             _plane("state_in", state_in, shape), _plane("state_out", state_out, shape), 0, 0, 0, 0]
-    w = _workspace(_DECAY.pack(*args), 0)
+    w = _workspace(_packed(_DECAY, *args), 0)
     if w is not None:
         args[-2:] = w.data_ptr(), w.numel()
-    _call("ob_decay_attention", lib().ob_decay_attention(s, _DECAY.pack(*args)))
+    _call("ob_decay_attention", lib().ob_decay_attention(s, _packed(_DECAY, *args)))
     return o
 
 
@@ -165,10 +174,10 @@ def decay_attention_grad(q, k, v, log_decay, offsets, do, scale: Optional[float]
             *_rows("v", v, (tokens, kv_heads, dv), q.dtype), *_rows("do", do, (tokens, heads, dv), q.dtype),
             dq.data_ptr(), heads * dk, dk, gk.data_ptr(), kv_heads * dk, dk, gv.data_ptr(), kv_heads * dv, dv,
             _plane("state_in", state_in, shape), 0, _plane("dstate_out", dstate_out, shape), _plane("dstate_in", dstate_in, shape), 0, 0]
-    w = _workspace(_DECAY.pack(*args), 1)
+    w = _workspace(_packed(_DECAY, *args), 1)
     if w is not None:
         args[-2:] = w.data_ptr(), w.numel()
-    _call("ob_decay_attention_grad", lib().ob_decay_attention_grad(s, _DECAY.pack(*args)))
+    _call("ob_decay_attention_grad", lib().ob_decay_attention_grad(s, _packed(_DECAY, *args)))
     return dq, gk, gv
 
 
@@ -180,8 +189,8 @@ def decay_attention_step(q, k, v, log_decay, state, scale: Optional[float] = Non
     if state is None:
         raise ObError(OB_E_ARG, "no state")
     o = q.new_empty((tokens, heads, dv))
-    _call("ob_decay_attention_step", lib().ob_decay_attention_step(s, _DECAY.pack(
-        code, heads, kv_heads, dk, dv, tokens, tokens, dk ** -0.5 if scale is None else scale, _decay(log_decay, heads), 0,
+    _call("ob_decay_attention_step", lib().ob_decay_attention_step(s, _packed(
+        _DECAY, code, heads, kv_heads, dk, dv, tokens, tokens, dk ** -0.5 if scale is None else scale, _decay(log_decay, heads), 0,
         *_rows("q", q, (tokens, heads, dk), dtype), *_rows("k", k, (tokens, kv_heads, dk), dtype), *_rows("v", v, (tokens, kv_heads, dv), dtype),
         o.data_ptr(), heads * dv, dv, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, _plane("state", state, (tokens, heads, dk, dv)), 0, 0, 0, 0)))
     return o
@@ -223,8 +232,8 @@ def token_logprobs(scores, labels, top: int = 0) -> TokenLogprobs:
     h, stats = lp.new_empty(rows), lp.new_empty((2, rows))
     top_lp, top_id = lp.new_empty((rows, top)), labels.new_empty((rows, top), dtype=torch.int32)
     at = stats.data_ptr()
-    _call("ob_token_logprobs", lib().ob_token_logprobs(s, _SCORES.pack(
-        code, wide, rows, classes, top, 0, scores.data_ptr(), scores.stride(0), labels.data_ptr(), lp.data_ptr(), h.data_ptr(), at, at + 4 * rows,
+    _call("ob_token_logprobs", lib().ob_token_logprobs(s, _packed(
+        _SCORES, code, wide, rows, classes, top, 0, scores.data_ptr(), scores.stride(0), labels.data_ptr(), lp.data_ptr(), h.data_ptr(), at, at + 4 * rows,
         top_lp.data_ptr(), top_id.data_ptr(), 0, 0, 0, 0)))
     return TokenLogprobs(lp, h, top_lp, top_id, stats)
 
@@ -242,8 +251,8 @@ def token_logprobs_grad(scores, labels, result: TokenLogprobs, dlogprob=None, de
             raise ObError(OB_E_DIM, f"{name}: a contiguous fp32 tensor of shape {shape} is wanted, not {t.dtype} {tuple(t.shape)}")
     d = scores.new_empty((rows, classes))
     at = result.row_stats.data_ptr()
-    _call("ob_token_logprobs_grad", lib().ob_token_logprobs_grad(s, _SCORES.pack(
-        code, wide, rows, classes, 0, 0, scores.data_ptr(), scores.stride(0), labels.data_ptr(), result.logprob.data_ptr(), result.entropy.data_ptr(),
+    _call("ob_token_logprobs_grad", lib().ob_token_logprobs_grad(s, _packed(
+        _SCORES, code, wide, rows, classes, 0, 0, scores.data_ptr(), scores.stride(0), labels.data_ptr(), result.logprob.data_ptr(), result.entropy.data_ptr(),
         at, at + 4 * rows, 0, 0, 0 if dlogprob is None else dlogprob.data_ptr(),
         0 if dentropy is None else dentropy.data_ptr(), d.data_ptr(), classes)))
     return d
