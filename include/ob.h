@@ -401,7 +401,8 @@ typedef struct ob_tensor {
 int ob_clip_workspace(const ob_tensor *tensors, int n, uint64_t *bytes);
 /* norm (device, one float) = the square root of the sum of all gradients' squares, and with f = min(1, max_norm / norm)
  * every parameter becomes parameter - lr * f * gradient; without parameters every gradient becomes f * gradient.  max_norm may be
- * infinite: nothing is clipped.  A norm that is NaN makes NaN of what is written.  `tensors` is host memory. */
+ * infinite: nothing is clipped.  A norm that is NaN makes NaN of what is written.  `tensors` is host memory.  Arrays that are
+ * written may not share memory with each other (OB_E_ARG), nor parameters with the gradients of others. */
 int ob_clip_step(void *hip_stream, const ob_tensor *tensors, int n, double max_norm, double lr, float *norm, void *workspace,
                  uint64_t workspace_bytes);
 

@@ -2,6 +2,10 @@
 #include "ob_dev.h"
 #include "ob_ctx.h"
 
+#include <algorithm>
+#include <memory>
+#include <new>
+
 namespace {
 
 constexpr int TENSORS = 128;         // of one launch: the table travels in the kernel's arguments
@@ -154,11 +158,39 @@ __global__ void __launch_bounds__(256) k_update(const UpdateArgs A)
     }
 }
 
+constexpr int SIZE[3] = {4, 2, 2};   // bytes of an element
+
+// Whether two of the arrays that a call writes share memory: 0 no, 1 yes, -1 no room to find out.  Lists mostly rise in memory already.
+int share_memory(const ob_tensor *t, int n)
+{
+    struct Range { uintptr_t lo, hi; };
+    auto range = [](const ob_tensor &x) {
+        const uintptr_t lo = (uintptr_t)(x.param ? x.param : x.grad);
+        return Range{lo, lo + (uintptr_t)x.n * SIZE[x.param ? x.param_type : x.grad_type]};
+    };
+    uintptr_t end = 0;
+    int i = 0, count = 0;
+    for (; i < n; ++i) {
+        if (!t[i].n) continue;
+        const Range r = range(t[i]);
+        if (r.lo < end) break;
+        end = r.hi;
+    }
+    if (i == n) return 0;
+    std::unique_ptr<Range[]> all(new (std::nothrow) Range[n]);
+    if (!all) return -1;
+    for (i = 0; i < n; ++i)
+        if (t[i].n) all[count++] = range(t[i]);
+    std::sort(all.get(), all.get() + count, [](const Range &a, const Range &b) { return a.lo < b.lo; });
+    for (i = 1; i < count; ++i)
+        if (all[i].lo < all[i - 1].hi) return 1;
+    return 0;
+}
+
 // The table of the tensors from `i` on; arrays that adjoin in memory (views of one buffer) become one entry.  Returns the first tensor that
 // found no place.
 int fill(UpdateArgs &A, const ob_tensor *t, int i, int count)
 {
-    static const int size[3] = {4, 2, 2};
     A.n = 0, A.cum[0] = 0;
     u64 chunks = 0;
     for (; i < count; ++i) {
@@ -167,8 +199,8 @@ int fill(UpdateArgs &A, const ob_tensor *t, int i, int count)
         if (A.n) {
             Entry &e = A.t[A.n - 1];
             const i64 n = e.n_types >> 4;
-            if ((e.n_types & 15) == types && (char *)e.g + n * size[t[i].grad_type] == (char *)t[i].grad &&
-                (t[i].param == nullptr ? e.p == nullptr : (char *)e.p + n * size[t[i].param_type] == (char *)t[i].param)) {
+            if ((e.n_types & 15) == types && (char *)e.g + n * SIZE[t[i].grad_type] == (char *)t[i].grad &&
+                (t[i].param == nullptr ? e.p == nullptr : (char *)e.p + n * SIZE[t[i].param_type] == (char *)t[i].param)) {
                 const i64 all = n + t[i].n;
                 chunks = A.cum[A.n - 1] + (u64)((all + CHUNK - 1) / CHUNK);
                 e.n_types = all << 4 | types;
@@ -215,6 +247,9 @@ int ob_clip_step(void *hip_stream, const ob_tensor *tensors, int n, double max_n
         (t.param ? params : none) = true;
     }
     if (params && none) return ops_fail(OB_E_ARG, "ob_clip_step: parameters for some of the gradients only");
+    if (const int shared = share_memory(tensors, n))
+        return shared < 0 ? ops_fail(OB_E_OOM, "ob_clip_step: no host memory for %d tensors", n)
+                          : ops_fail(OB_E_ARG, "ob_clip_step: two %s share memory", params ? "parameters" : "gradients");
     hipStream_t s = (hipStream_t)hip_stream;
     UpdateArgs A;
     A.part = (double *)workspace, A.part_first = 0, A.part_count = 0;
