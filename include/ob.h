@@ -357,10 +357,10 @@ typedef struct ob_decay {
 
 /* bytes of workspace that ob_decay_attention (grad = 0) or ob_decay_attention_grad (grad = 1) needs for these sizes and offsets */
 int ob_decay_workspace(const ob_decay *p, int grad, uint64_t *bytes);
-/* o and state_out of whole sequences.  state_out may not overlap state_in. */
+/* o and state_out of whole sequences.  state_out may not share memory with state_in (OB_E_ARG). */
 int ob_decay_attention(void *hip_stream, const ob_decay *p);
 /* Gradients with respect to q, k, v and state_in from those with respect to o and state_out.  Keys and values that heads
- * share get the sum over the group, made in fp32. */
+ * share get the sum over the group, made in fp32.  dstate_in may not share memory with state_in and dstate_out (OB_E_ARG). */
 int ob_decay_attention_grad(void *hip_stream, const ob_decay *p);
 /* One new token of each of n_seqs sequences (tokens = n_seqs, row b is sequence b): state_out is read, updated in place, and o written.
  * offsets and workspace are not looked at. */

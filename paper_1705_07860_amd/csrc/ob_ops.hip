@@ -228,6 +228,13 @@ static void fill_units(ScanArgs &A, const ob_decay *p, int first_seq, int segmen
     A.n_units = A.n_cut + n_seqs - A.n_split;
 }
 
+// workgroups read the states that enter while others write those that leave
+static bool share_memory(const ob_decay *p, const float *x, const float *y)
+{
+    const uintptr_t a = (uintptr_t)x, b = (uintptr_t)y, bytes = (uintptr_t)p->n_seqs * p->heads * p->dk * p->dv * sizeof(float);
+    return a && b && a < b + bytes && b < a + bytes;
+}
+
 static int pad_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : 128; }
 
 // bytes of the states of segments, at most over the launches
@@ -299,6 +306,7 @@ int ob_decay_attention(void *hip_stream, const ob_decay *p)
 {
     if (int rc = check_decay(p, "ob_decay_attention", true)) return rc;
     if (!p->n_seqs) return OB_OK;
+    if (share_memory(p, p->state_in, p->state_out)) return ops_fail(OB_E_ARG, "ob_decay_attention: state_in and state_out share memory");
     const int segment = segment_of(p, 1), group = p->heads / p->kv_heads;
     const size_t need = slot_bytes(p, segment, 1);
     if (need > p->workspace_bytes || (need && !p->workspace))
@@ -320,6 +328,8 @@ int ob_decay_attention_grad(void *hip_stream, const ob_decay *p)
     if (int rc = check_decay(p, "ob_decay_attention_grad", true)) return rc;
     if (!p->n_seqs) return OB_OK;
     if (p->tokens && (!p->dq.data || !p->dk_rows.data || !p->dv_rows.data)) return ops_fail(OB_E_ARG, "ob_decay_attention_grad: null array");
+    if (share_memory(p, p->state_in, p->dstate_in) || share_memory(p, p->dstate_out, p->dstate_in))
+        return ops_fail(OB_E_ARG, "ob_decay_attention_grad: dstate_in shares memory with a state that is read");
     hipStream_t s = (hipStream_t)hip_stream;
     const int scans = grad_scans(p), segment = segment_of(p, scans), group = p->heads / p->kv_heads;
     const size_t slots = slot_bytes(p, segment, scans), need = slots + part_bytes(p);

@@ -129,7 +129,7 @@ def decay_attention(q, k, v, log_decay, offsets, scale: Optional[float] = None, 
     """o [tokens, heads, dv] for q [tokens, heads, dk], k [tokens, kv_heads, dk], v [tokens, kv_heads, dv], log_decay [heads] (fp32, <= 0).
 
     Sequence b has the tokens offsets[b] .. offsets[b + 1] - 1 (host numbers).  state_in, state_out [sequences, heads, dk, dv] (fp32,
-    contiguous, two tensors): the state before the first token (zeros without), and the one behind the last, which is written if given.
+    contiguous, apart in memory): the state before the first token (zeros without), and the one behind the last, which is written if given.
     scale: dk ** -0.5 if not given.  Heads may have any strides; the elements of a head are neighbours."""
     s = _stream(q, k, v, log_decay, state_in, state_out)
     tokens, heads, kv_heads, dk, dv = _widths(q, k, v)
@@ -138,8 +138,6 @@ def decay_attention(q, k, v, log_decay, offsets, scale: Optional[float] = None, 
     n = len(off) - 1
     shape = (n, heads, dk, dv)
     o = q.new_empty((tokens, heads, dv))
-    if state_in is not None and state_out is not None and state_in.data_ptr() == state_out.data_ptr() and n:
-        raise ObError(OB_E_ARG, "state_in and state_out are the same memory")
     args = [code, heads, kv_heads, dk, dv, n, tokens, dk ** -0.5 if scale is None else scale, _decay(log_decay, heads), off.buffer_info()[0],
             *_rows("q", q, (tokens, heads, dk), q.dtype), *_rows("k", k, (tokens, kv_heads, dk), q.dtype),
             *_rows("v", v, (tokens, kv_heads, dv), q.dtype), o.data_ptr(), heads * dv, dv, *_NO_ROWS, *_NO_ROWS, *_NO_ROWS,
@@ -165,10 +163,6 @@ def decay_attention_grad(q, k, v, log_decay, offsets, do, scale: Optional[float]
     dq = q.new_empty((tokens, heads, dk))
     gk = q.new_empty((tokens, kv_heads, dk))
     gv = q.new_empty((tokens, kv_heads, dv))
-    if dstate_in is not None and n:
-        for name, t in (("state_in", state_in), ("dstate_out", dstate_out)):
-            if t is not None and t.data_ptr() == dstate_in.data_ptr():
-                raise ObError(OB_E_ARG, f"{name} and dstate_in are the same memory")
     args = [code, heads, kv_heads, dk, dv, n, tokens, dk ** -0.5 if scale is None else scale, _decay(log_decay, heads), off.buffer_info()[0],
             *_rows("q", q, (tokens, heads, dk), q.dtype), *_rows("k", k, (tokens, kv_heads, dk), q.dtype),
             *_rows("v", v, (tokens, kv_heads, dv), q.dtype), *_rows("do", do, (tokens, heads, dv), q.dtype),
