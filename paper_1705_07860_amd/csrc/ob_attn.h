@@ -494,8 +494,8 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
     const bool give = !STATE_ONLY && s_out && u.part == u.parts - 1;
     const bool exact = STATE_ONLY ? A.exact_state : give;
     bool have = from_slot || from_user;         // the state may hold something
-    int s_scale = 0;                            // fp16: S is held times held = 2^s_scale
-    float held = 1.0f;
+    int s_scale = 0;                            // fp16: S (STATE_ONLY: what is added to it) is held times held = 2^s_scale
+    float held = 1.0f, loose = 1.0f;            // loose: STATE_ONLY, 2^-s_scale
 
     // powers of the decay, and what a whole chunk's rows weigh in the state behind it: those of a chunk of n rows lie CH - n further on
     if (tid < 64) {
@@ -651,7 +651,7 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
                     }
                     if (bits) {
                         const int e = min(max(fit_exponent(bits), -100 - s_scale), 100 - s_scale);
-                        keep *= two_to(e), held *= two_to(e), s_scale += e;
+                        keep *= two_to(e), held *= two_to(e), loose *= two_to(-e), s_scale += e;
                     }
                 }
 #pragma unroll
@@ -662,7 +662,7 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
             float behind = 1.0f;
             if constexpr (STATE_ONLY) {
                 behind = decay_power(decay, at);
-                if constexpr (Q::SCALED) behind *= two_to(-s_scale);
+                if constexpr (Q::SCALED) behind *= loose;
                 else
 #pragma unroll
                     for (int ct = 0; ct < NC; ++ct) x0[ct] *= behind, x1[ct] *= behind;
@@ -706,6 +706,12 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
                             S[ct][dt + 1] = Q::mma(z0, z1, t0[ct][m], t1[ct][m], S[ct][dt + 1]);
                         }
             }
+            // the sums stay on this side of the loop's branches, behind which the compiler may place them too near to the products that they add
+            if constexpr (STATE_ONLY && Q::SCALED)
+#pragma unroll
+                for (int ct = 0; ct < NC; ++ct)
+#pragma unroll
+                    for (int dt = 0; dt < ND; ++dt) asm volatile("" : "+v"(S[ct][dt]));
             if constexpr (Q::SPLIT > 2) {
                 if (exact) {
 #pragma unroll
