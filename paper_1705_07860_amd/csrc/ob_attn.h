@@ -378,7 +378,9 @@ template <typename T, int DA, int DC, bool FULL> constexpr int scan_occupancy()
 
 // One workgroup walks the chunks of one unit for one head.  A wave has NC blocks of 16 columns of S and y and holds its part of S in fp32 in the
 // accumulators throughout; the scores inside a chunk are made once, a block a wave, and pass through LDS.  What is rounded to 16 bits: scores
-// (after decay) and the state where it is multiplied with a_i, one rounding each like that of y itself.  What is added to the state is not:
+// (after decay) and the state where it is multiplied with a_i, one rounding each like that of y itself, which over a chunk's rows and columns
+// average out to 1.4 times y's own error; not in a unit's last chunk, where both are two terms (0.8% of 48 ragged prompts in fp16; in every chunk
+// second terms of scores would cost fp16 of 128 x 128 its third workgroup).  What is added to the state is not:
 // decayed rows of c enter as SPLIT terms whose sum holds 22 (fp16) or 24 bits (bf16; two terms, 16 bits, where the state itself is not
 // returned and only feeds 16-bit outputs).
 // Chunks of 32 rows: a state of 128 x 128 takes 64 registers a lane of four waves, and a chunk's rows twice in LDS leave room for two or three
@@ -525,6 +527,10 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
         const int from = BUF == 2 ? half : 0;
         const T *sa = s_x + from * HALF + TA, *sb = s_x + from * HALF + TB, *sc = s_x + from * HALF + TC;
         const u32 at_half = from * (HALF * 2);
+        // In the last chunk of a unit, the only one of a short sequence, scores and the state enter products as two terms: a score is one rounding for all
+        // columns of a row, and the roundings of few rows do not average out (errors of up to twice the output's own).  Second
+        // terms of scores lie in the half of the buffers that is free then.
+        Frag *s_low = (Frag *)(s_x + (BUF == 2 ? half ^ 1 : 0) * HALF);
         auto a_rows = [&](int r0, int k0) -> Frag {
             if constexpr (DIRECT) return direct_rows(row_lane + at_half, (TA + r0 * DA) * 2, k0);
             else return rows_frag(sa, LA, r0, k0, lane);
@@ -570,23 +576,28 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
                     }
                     if (lane == 0) s_exp[half][t] = e;
                 }
-                s_p[half][t][lane] = to_frag<T>(x);
+                const Frag p = to_frag<T>(x);
+                s_p[half][t][lane] = p;
+                if (Q::SPLIT > 1 && left <= 0) s_low[t * 64 + lane] = to_frag<T>(x - from_frag<T>(p));
             }
             // what the state before the chunk gives
             if (have) {
-                auto from_state = [&](auto scaled, float by) {
+                auto from_state = [&](auto scaled, auto low, float by) {
 #pragma unroll
                     for (int dt = 0; dt < ND; dt += 2) {
                         const Frag a0 = a_rows(0, dt * 16), a1 = a_rows(0, dt * 16 + 16);
                         const Frag b0 = a_rows(16, dt * 16), b1 = a_rows(16, dt * 16 + 16);
 #pragma unroll
                         for (int ct = 0; ct < NC; ++ct) {
-                            const Frag s0 = to_frag<T>(scaled ? S[ct][dt] * by : S[ct][dt]), s1 = to_frag<T>(scaled ? S[ct][dt + 1] * by : S[ct][dt + 1]);
+                            const f4 x0 = scaled ? S[ct][dt] * by : S[ct][dt], x1 = scaled ? S[ct][dt + 1] * by : S[ct][dt + 1];
+                            Frag s0 = to_frag<T>(x0), s1 = to_frag<T>(x1);
+                            if (low) s0 = to_frag<T>(x0 - from_frag<T>(s0)), s1 = to_frag<T>(x1 - from_frag<T>(s1));
                             acc[ct][0] = Q::mma(s0, s1, a0, a1, acc[ct][0]);
                             acc[ct][1] = Q::mma(s0, s1, b0, b1, acc[ct][1]);
                         }
                     }
                 };
+                float by = 1.0f;
                 if constexpr (Q::SCALED) {
                     by_state = two_to(-s_scale);
                     // As it is where the largest element is one that leaves 13 binary places below it, else times a power of two.  The largest
@@ -612,12 +623,13 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
                             bits = wave_max(bits);
                         }
                         const int e = fit_exponent(bits);
-                        by_state = two_to(-e - s_scale);
-                        from_state(std::true_type(), two_to(e));
+                        by_state = two_to(-e - s_scale), by = two_to(e);
+                        from_state(std::true_type(), std::false_type(), by);
                     } else
-                        from_state(std::false_type(), 1.0f);
+                        from_state(std::false_type(), std::false_type(), by);
                 } else
-                    from_state(std::false_type(), 1.0f);
+                    from_state(std::false_type(), std::false_type(), by);
+                if (Q::SPLIT > 1 && left <= 0) from_state(std::bool_constant<Q::SCALED>(), std::true_type(), by);
             }
         }
         // the state behind the chunk
@@ -743,13 +755,19 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
             const float into0 = sy * s_power[l + once] * by_state, into1 = sy * s_power[16 + l + once] * by_state;
             const bool p_scaled = Q::SCALED && __builtin_amdgcn_readfirstlane(s_exp[half][0] | s_exp[half][1] | s_exp[half][2]);
             const Frag p00 = s_p[half][0][lane], p10 = s_p[half][1][lane], p11 = s_p[half][2][lane];
+            Frag r00 = none, r10 = none, r11 = none;
+            if (Q::SPLIT > 1 && left <= 0) r00 = s_low[lane], r10 = s_low[64 + lane], r11 = s_low[128 + lane];
 #pragma unroll
             for (int ct = 0; ct < NC; ++ct) {
                 acc[ct][0] *= into0, acc[ct][1] *= into1;
                 if (Q::SCALED && p_scaled) {
                     const f4 zero = {0.f, 0.f, 0.f, 0.f};
-                    acc[ct][0] += Q::mma(v0[ct], none, p00, none, zero) * two_to(-s_exp[half][0]);
-                    acc[ct][1] += Q::mma(v0[ct], none, p10, none, zero) * two_to(-s_exp[half][1]) + Q::mma(v1[ct], none, p11, none, zero) * two_to(-s_exp[half][2]);
+                    acc[ct][0] += Q::mma(v0[ct], v0[ct], p00, r00, zero) * two_to(-s_exp[half][0]);
+                    acc[ct][1] += Q::mma(v0[ct], v0[ct], p10, r10, zero) * two_to(-s_exp[half][1]) + Q::mma(v1[ct], v1[ct], p11, r11, zero) * two_to(-s_exp[half][2]);
+                } else if constexpr (Q::SPLIT > 1) {
+                    acc[ct][0] = Q::mma(v0[ct], v0[ct], p00, r00, acc[ct][0]);
+                    acc[ct][1] = Q::mma(v0[ct], v1[ct], p10, p11, acc[ct][1]);
+                    if (left <= 0) acc[ct][1] = Q::mma(v0[ct], v1[ct], r10, r11, acc[ct][1]);
                 } else {
                     acc[ct][0] = Q::mma(v0[ct], none, p00, none, acc[ct][0]);
                     acc[ct][1] = Q::mma(v0[ct], v1[ct], p10, p11, acc[ct][1]);
