@@ -167,12 +167,9 @@ __device__ __forceinline__ int finite_bits(float x)
     const int b = bits_of(x);
     return b < BITS_INF ? b : 0;
 }
-// the power of two that brings a magnitude (its bits) to 2^11 .. 2^12, as an exponent: products keep 26 binary places below the largest
-__device__ __forceinline__ int fit_exponent(int bits)
-{
-    const int e = (bits >> 23) - 127;
-    return 11 - (e < -60 ? -60 : e > 60 ? 60 : e);
-}
+// the power of two that brings a finite magnitude (its bits) to 2^11 .. 2^12, as an exponent: products keep 26 binary places below the largest.
+// -116 .. 126: itself and its inverse are normal numbers; what is below 2^-115 stays smaller.
+__device__ __forceinline__ int fit_exponent(int bits) { return 11 - max((bits >> 23) - 127, -115); }
 __device__ __forceinline__ float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
 __device__ __forceinline__ float two_to(int e) { return __builtin_amdgcn_ldexpf(1.0f, e); }
 
@@ -652,18 +649,17 @@ __global__ void __launch_bounds__(64 * scan_waves<DC>(), (scan_occupancy<T, DA, 
                 // held times 2^s_scale, the largest between 2^11 and 2^14: the second term has its bits then down to 2^-24 of the largest
                 most_x *= held;
                 if (__builtin_amdgcn_ballot_w64(most_x > 16384.0f) || !__builtin_amdgcn_ballot_w64(most_x >= 2048.0f)) {
-                    int bits = wave_max(bits_of(most_x));
-                    if (bits >= BITS_INF) {
-                        bits = 0;
+                    // of the rows as they are: held, they may have left fp32's range where the power changes much, as it does when rows of zeros
+                    // follow a fast decay
+                    int bits = 0;
 #pragma unroll
-                        for (int ct = 0; ct < NC; ++ct)
+                    for (int ct = 0; ct < NC; ++ct)
 #pragma unroll
-                            for (int r = 0; r < 4; ++r) bits = max(bits, max(finite_bits(x0[ct][r] * held), finite_bits(x1[ct][r] * held)));
-                        bits = wave_max(bits);
-                    }
+                        for (int r = 0; r < 4; ++r) bits = max(bits, max(finite_bits(x0[ct][r]), finite_bits(x1[ct][r])));
+                    bits = wave_max(bits);
                     if (bits) {
-                        const int e = min(max(fit_exponent(bits), -100 - s_scale), 100 - s_scale);
-                        keep *= two_to(e), held *= two_to(e), loose *= two_to(-e), s_scale += e;
+                        const int to = min(max(fit_exponent(bits), -100), min(100, s_scale + 120));
+                        keep *= two_to(to - s_scale), held = two_to(to), loose = two_to(-to), s_scale = to;
                     }
                 }
 #pragma unroll
