@@ -170,7 +170,6 @@ __device__ __forceinline__ int finite_bits(float x)
 // the power of two that brings a finite magnitude (its bits) to 2^11 .. 2^12, as an exponent: products keep 26 binary places below the largest.
 // -116 .. 126: itself and its inverse are normal numbers; what is below 2^-115 stays smaller.
 __device__ __forceinline__ int fit_exponent(int bits) { return 11 - max((bits >> 23) - 127, -115); }
-__device__ __forceinline__ float uniform(float x) { return __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, x))); }
 __device__ __forceinline__ float two_to(int e) { return __builtin_amdgcn_ldexpf(1.0f, e); }
 
 // ---- rows of a chunk -------------------------------------------------------------------------------------------------
