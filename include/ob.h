@@ -314,7 +314,7 @@ int ob_test_gemm(ob_ctx *ctx, int M, int N, int K, const float *A, const float *
  * nothing from the host and wait for nothing, so that they may be captured into a HIP graph (what lies in host memory,
  * offsets and tables of tensors, is read during the call).  Scratch memory is the caller's (`workspace`, 256-byte
  * aligned; it may be used again once the stream has passed the call).  Sums, states, norms and statistics are held in 32
- * bits or more.  The same inputs give the same bits.  Message of a failed call: ob_last_error(NULL). */
+ * bits or more.  The same call on the same inputs gives the same bits.  Message of a failed call: ob_last_error(NULL). */
 
 /* element types */
 #define OB_TYPE_FP32 0
@@ -334,7 +334,8 @@ typedef struct ob_rows {
  * on packed sequences: sequence b is the tokens offsets[b] .. offsets[b + 1] - 1, none allowed.  `heads` query heads share
  * kv_heads heads of keys and values, in groups of heads / kv_heads neighbours; every query head has a state.
  * log_decay is <= 0 (0: no decay; -inf: no memory).  A NaN or an infinity reaches its own sequence only, but may reach
- * outputs of up to 15 tokens before it, as the products inside a block of rows take it in. */
+ * outputs of up to 15 tokens before it, as the products inside a block of rows take it in.  In 16 bits scores and states are rounded where
+ * they enter a product (in sequences of up to 32 tokens only o itself is); in bf16 o may differ in its last bit with state_out from o without. */
 typedef struct ob_decay {
     int32_t type;                /* OB_TYPE_* of q, k, v, o and their gradients */
     int32_t heads, kv_heads;

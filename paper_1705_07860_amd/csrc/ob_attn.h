@@ -380,8 +380,8 @@ template <typename T, int DA, int DC, bool FULL> constexpr int scan_occupancy()
 // decayed rows of c enter as SPLIT terms whose sum holds 22 (fp16) or 24 bits (bf16; two terms, 16 bits, where the state itself is not
 // returned and only feeds 16-bit outputs).
 // Chunks of 32 rows: a state of 128 x 128 takes 64 registers a lane of four waves, and a chunk's rows twice in LDS leave room for two or three
-// workgroups a compute unit; with 64 rows registers spill (1050 us for the 241 below).  128 x 128: bf16, 65 536 tokens of 16 heads 241 us,
-// 4.5 TB/s (a copy reaches 4.7), and 122 for the states of the segments; fp16, 43 628 tokens of 32 heads over 8 of keys 315 us, 3.5 TB/s.  Two
+// workgroups a compute unit; with 64 rows registers spill (1050 us for the 241 below).  128 x 128: bf16, 65 536 tokens of 16 heads 242 us,
+// 4.5 TB/s (a copy reaches 4.7), and 123 for the states of the segments; fp16, 43 628 tokens of 32 heads over 8 of keys 317 us, 3.45 TB/s.  Two
 // chunks take a compute unit 6400 clocks in bf16: the vector units are busy 2800 of them, the matrix units 1760, LDS 1450; what is left are
 // memory and their latencies.  Loads a chunk further ahead, reads of LDS ahead of their products, eight waves of 16 columns, rows of y put
 // together in LDS, one decay for several chunks: within 2%.  y stored past the caches: 608 us for the 366 of both passes, since a wave has

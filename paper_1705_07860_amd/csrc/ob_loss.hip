@@ -46,7 +46,8 @@ constexpr int KEPT = 512;            // candidates for the most likely classes
 // For the most likely classes each lane of the first wave has the largest elements of two groups of threads; the top-th largest of these 128,
 // found bit by bit from how many reach each prefix, is a bound that at least `top` elements reach and, unless many are equal, few more do: some 8
 // for 8, 37 for 32, 89 for 64.  The few threads that have any read theirs again, out of the caches, and put them to a list, where they are
-// ranked by (score, lower class first).  If too many reach the bound, they are picked one by one.
+// ranked by (score, lower class first).  If too many reach the bound, as in rows of equal scores, they are picked one by one, the row read again for
+// each (8192 rows of 32 000 equal bf16 scores: 8 classes 785 us, 64 classes 5.1 ms).
 // 8192 rows of 32 000 bf16: without classes 89 us, 5.9 TB/s; 8 classes 115, 64 138 (with one group a lane 740: too many reach the least of 64).
 // Slower for 8: ranks of the groups by comparing each with each 123, all threads reading again 147, the row kept in LDS 174 (room for two
 // workgroups a compute unit), in registers 561.  Comparing differences to the maximum so far in place of the elements saves a third
@@ -59,7 +60,8 @@ template <typename T, int THREADS> __global__ void __launch_bounds__(THREADS) k_
     __shared__ float s_red[3][WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, row = A.first + (int)blockIdx.x;
     const T *first = (const T *)A.x + row * A.x_row;
-    // vectors from the first place of 16 bytes on (rows of 50 257 bf16: 82 us for 93); what lies before it goes one by one
+    // vectors from the first place of 16 bytes on (4096 rows of 50 257 bf16 by
+    // themselves, inputs that take turns: 83 us for 93); what lies before it goes one by one
     const int head = min((int)(-(uintptr_t)first & 15) / (int)sizeof(T), A.classes), classes = A.classes - head;
     const T *x = first + head;
     const int full = classes / VEC, vecs = (classes + VEC - 1) / VEC;
@@ -320,7 +322,8 @@ struct ScoreGradArgs {
 };
 
 // dx_c = a (1[c = y] - p_c) - b p_c (log p_c + H).  Elementwise: a reading and a writing, rows from the last on, since the last ones that the
-// forward pass read are still in the last-level cache.  4096 rows of 50 257 bf16: 156 us, 5.3 TB/s (and 103 us for the pass before it).
+// forward pass read are still in the last-level cache.  4096 rows of 50 257 bf16: 156 us, 5.3 TB/s (and 104 us for the
+// forward pass before it, which finds the caches full of the last gradient; by itself that takes 83 to 88).
 template <typename T> __global__ void __launch_bounds__(256) k_logprobs_grad(const ScoreGradArgs A)
 {
     constexpr int VEC = 16 / (int)sizeof(T), U = 4;

@@ -142,10 +142,12 @@ def decay_attention(q, k, v, log_decay, offsets, scale: Optional[float] = None, 
             *_rows("q", q, (tokens, heads, dk), q.dtype), *_rows("k", k, (tokens, kv_heads, dk), q.dtype),
             *_rows("v", v, (tokens, kv_heads, dv), q.dtype), o.data_ptr(), heads * dv, dv, *_NO_ROWS, *_NO_ROWS, *_NO_ROWS,
             _plane("state_in", state_in, shape), _plane("state_out", state_out, shape), 0, 0, 0, 0]
-    w = _workspace(_packed(_DECAY, *args), 0)
+    record = _packed(_DECAY, *args)
+    w = _workspace(record, 0)
     if w is not None:
         args[-2:] = w.data_ptr(), w.numel()
-    _call("ob_decay_attention", lib().ob_decay_attention(s, _packed(_DECAY, *args)))
+        record = _packed(_DECAY, *args)
+    _call("ob_decay_attention", lib().ob_decay_attention(s, record))
     return o
 
 
@@ -168,10 +170,12 @@ def decay_attention_grad(q, k, v, log_decay, offsets, do, scale: Optional[float]
             *_rows("v", v, (tokens, kv_heads, dv), q.dtype), *_rows("do", do, (tokens, heads, dv), q.dtype),
             dq.data_ptr(), heads * dk, dk, gk.data_ptr(), kv_heads * dk, dk, gv.data_ptr(), kv_heads * dv, dv,
             _plane("state_in", state_in, shape), 0, _plane("dstate_out", dstate_out, shape), _plane("dstate_in", dstate_in, shape), 0, 0]
-    w = _workspace(_packed(_DECAY, *args), 1)
+    record = _packed(_DECAY, *args)
+    w = _workspace(record, 1)
     if w is not None:
         args[-2:] = w.data_ptr(), w.numel()
-    _call("ob_decay_attention_grad", lib().ob_decay_attention_grad(s, _packed(_DECAY, *args)))
+        record = _packed(_DECAY, *args)
+    _call("ob_decay_attention_grad", lib().ob_decay_attention_grad(s, record))
     return dq, gk, gv
 
 
